@@ -501,8 +501,8 @@ int fstc_label_logprob_grad(const void *logits, int dtype, uint64_t rows, uint32
  *   loss = mean over p of -(1 - e) log sigmoid(margin) - e log sigmoid(-margin)
  * with e = label_smoothing in [0, 0.5).  seq_logprob [2 pairs] receives L,
  * seq_weight [2 pairs] the loss's derivatives in L (the weights of
- * fstc_label_logprob_grad with rows_per_weight = positions).  L is summed
- * pairwise in 32 bits; margins are those of the returned L.
+ * fstc_label_logprob_grad with rows_per_weight = positions).  Sums,
+ * margins, loss and weights are formed in 64 bits and rounded to 32 once.
  */
 int fstc_preference_loss(const float *logprob, uint64_t pairs, uint64_t positions, const float *ref,
                          float beta, float label_smoothing, float *loss, float *seq_logprob,
