@@ -503,6 +503,10 @@ int fstc_label_logprob_grad(const void *logits, int dtype, uint64_t rows, uint32
  * seq_weight [2 pairs] the loss's derivatives in L (the weights of
  * fstc_label_logprob_grad with rows_per_weight = positions).  Sums,
  * margins, loss and weights are formed in 64 bits and rounded to 32 once.
+ * A sequence with a label that is not allowed has L = -inf: its pair's margin
+ * is infinite, the term that e = 0 leaves out is 0, the weights are finite.  Where
+ * infinities cancel (both sequences of a pair, or a sequence and its reference), the margin has
+ * no value: it is NaN, and the pair adds 0 to the mean and has weights 0.
  */
 int fstc_preference_loss(const float *logprob, uint64_t pairs, uint64_t positions, const float *ref,
                          float beta, float label_smoothing, float *loss, float *seq_logprob,

@@ -175,12 +175,17 @@ __global__ __launch_bounds__(kPrefNT) void k_preference(const float *lp, u64 pai
       if (lane == 0) seq_lp[s] = (float)side[k];
     }
     if (lane == 0) {
-      const double z = (double)beta * ((side[0] - (double)ref[p]) - (side[1] - (double)ref[pairs + p]));
+      const double apart = (side[0] - (double)ref[p]) - (side[1] - (double)ref[pairs + p]);
+      // no number, though all of its terms are: infinities that cancel
+      const bool none = isnan(apart) && !isnan(side[0]) && !isnan(side[1]) && !isnan(ref[p]) && !isnan(ref[pairs + p]);
+      const double z = beta == 0.f && !isnan(apart) ? 0.0 : (double)beta * apart;  // (0 times an infinity)
       const double eps = smoothing;
       // -log sigmoid(z) = max(-z, 0) + log(1 + exp(-|z|))
       const double soft = log1p(exp(-fabs(z)));
-      total += (1 - eps) * (fmax(-z, 0.0) + soft) + eps * (fmax(z, 0.0) + soft);
-      const double g = (eps - 1 / (1 + exp(z))) * (double)beta / (double)pairs;
+      double term = (1 - eps) * (fmax(-z, 0.0) + soft);
+      if (eps != 0) term += eps * (fmax(z, 0.0) + soft);  // (not 0 times an infinity)
+      if (!none) total += term;
+      const double g = none ? 0.0 : (eps - 1 / (1 + exp(z))) * (double)beta / (double)pairs;
       margin[p] = (float)z;
       seq_weight[p] = (float)g;
       seq_weight[pairs + p] = (float)-g;

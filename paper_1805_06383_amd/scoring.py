@@ -398,8 +398,11 @@ def preference_loss(logits: torch.Tensor, labels: torch.Tensor, ref_logprob: tor
     (loss, logprob [2 * pairs], margin [pairs]), float32: with L the sequences'
     log-probabilities, margin = beta * ((L - ref) of the preferred - (L - ref) of
     the other), loss = mean of -(1 - label_smoothing) log sigmoid(margin) -
-    label_smoothing log sigmoid(-margin).  The loss is differentiable in the
-    logits; logprob and margin are for reading."""
+    label_smoothing log sigmoid(-margin).  A sequence with a label of logit -inf has
+    log-probability -inf and its pair an infinite margin; where infinities cancel
+    (both sequences of a pair, or a sequence and its reference) the margin is NaN
+    and the pair adds nothing to the loss or its gradient.  The loss is
+    differentiable in the logits; logprob and margin are for reading."""
     if labels.ndim != 2 or labels.shape[0] % 2 or labels.shape[0] == 0:
         _refuse(f"labels: [2 * pairs, length], not {tuple(labels.shape)}")
     if tuple(logits.shape[:-1]) != tuple(labels.shape):

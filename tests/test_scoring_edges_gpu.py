@@ -34,3 +34,78 @@ def test_preference_margins_of_near_references(S, P, T, V, dtype):
     each = np.logaddexp(0, -z)
     near(loss, np.array(each.mean()), R.U32 * each.mean() * 1.01 + zoff.max() + 16 * U64 * each.mean(),
          "loss")
+
+
+@pytest.mark.parametrize("eps", [0.0, 0.1])
+@pytest.mark.parametrize("beta", [0.5, 0.0])
+def test_preference_of_disallowed_labels(S, eps, beta):
+    """Sequences of log-probability -inf.  Pairs: fine; the preferred one
+    disallowed; the other; both; the other, by the reference too; the other by the reference alone;
+    fine.  A margin without a value (infinities that cancel) is NaN, and its pair has no loss and
+    no weight; what the rest gives is what it gives alone."""
+    import torch
+    g = gen(60)
+    P, T, V, inf = 7, 4, 30, np.inf
+    x = normal(g, 2 * P, T, V, scale=2.0)
+    t = labels_of(g, (2 * P, T), V, pad=0.0)
+    ref = -10 * torch.rand(2 * P, generator=g, device="cuda")
+
+    def disallow(s):
+        x[s, 1, int(t[s, 1])] = -inf
+
+    disallow(1)
+    disallow(P + 2)
+    disallow(3), disallow(P + 3)
+    disallow(P + 4)
+    ref[P + 4] = -inf
+    ref[P + 5] = -inf
+    x.requires_grad_()
+    loss, seq, z = S.preference_loss(x, t, ref, beta=beta, label_smoothing=eps)
+    d, = torch.autograd.grad(loss, x)
+    b, e = float(np.float32(beta)), float(np.float32(eps))
+    lp, p, _ = R.logprob(R.f64(x), t.cpu().numpy())
+    L = lp.sum(1)
+    assert np.isneginf(L[[1, 3, P + 2, P + 3, P + 4]]).all()
+    near(seq, L, 1e-5 * np.where(np.isfinite(L), np.abs(L), 1), "sequences")
+    fine = np.array([0, 6])
+    with np.errstate(invalid="ignore"):
+        gain = L - R.f64(ref)
+    want = np.zeros(P)
+    want[fine] = b * (gain[fine] - gain[P + fine])
+    want[[1, 2, 5]] = [-inf, inf, -inf] if beta else 0.0
+    want[[3, 4]] = np.nan
+    near(z, want, 1e-4, "margin")
+    each = np.zeros(P)
+    some = ~np.isnan(want)
+    each[some] = (1 - e) * np.logaddexp(0, -want[some])
+    if eps:
+        each[some] += e * np.logaddexp(0, want[some])
+    near(loss.detach(), np.array(each.mean()), 1e-4, "loss")
+    with np.errstate(over="ignore"):
+        dz = np.where(some, (e - 1 / (1 + np.exp(np.where(some, want, 0)))) * b / P, 0.0)
+    w = np.repeat(np.concatenate([dz, -dz]), T).reshape(2 * P, T)
+    near(d, R.logprob_grad(R.f64(x), t.cpu().numpy(), w), 1e-5, "gradient")
+    # without the pairs of an infinite loss
+    some = torch.tensor([0, 2, 3, 4, 6], device="cuda")
+    both = torch.cat([some, P + some])
+    loss, _, _ = S.preference_loss(x.detach()[both], t[both], ref[both], beta=beta, label_smoothing=eps)
+    near(loss, np.array(each[some.cpu().numpy()].mean()), 1e-4, "loss of some")
+    # the pairs that always have a value, alone: their rows of the gradient
+    keep = torch.tensor([0, 6, P, P + 6], device="cuda")
+    y = x.detach()[keep].requires_grad_()
+    alone, = torch.autograd.grad(S.preference_loss(y, t[keep], ref[keep], beta=beta,
+                                                   label_smoothing=eps)[0], y)
+    near(d[keep], R.f64(alone) * 2 / P, 1e-6, "rows of the other pairs")
+
+
+def test_a_margin_of_nan_logits_is_seen(S):
+    """A pair without a value is left out only where infinities cancel: NaN stays NaN."""
+    import torch
+    x = torch.zeros(4, 2, 5, device="cuda")
+    x[1, 0, 3] = float("nan")
+    t = torch.ones(4, 2, dtype=torch.int32, device="cuda")
+    loss, seq, z = S.preference_loss(x, t, torch.zeros(4, device="cuda"))
+    assert torch.isnan(loss) and torch.isnan(seq[1]) and torch.isnan(z[1]) and torch.isfinite(z[0])
+    ref = torch.tensor([0.0, float("nan"), 0.0, 0.0], device="cuda")
+    loss, _, z = S.preference_loss(torch.zeros_like(x), t, ref)
+    assert torch.isnan(loss) and torch.isnan(z[1])
