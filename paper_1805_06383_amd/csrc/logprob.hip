@@ -90,7 +90,8 @@ __global__ __launch_bounds__(NT) void k_label_logprob(RowArgs a, const T *logits
     if (threadIdx.x == 0) {
       for (int w = 1; w < NT / kWave; ++w) r = join(r, s_part[w]);
       const bool none = r.m == -INFINITY && r.s == 0.f;
-      lp[row] = none ? -INFINITY : (to_f32(x[y]) - r.m) - logf(r.s);
+      // (in 64 bits, so that difference and logarithm are rounded once, together)
+      lp[row] = none ? -INFINITY : (float)(((double)to_f32(x[y]) - (double)r.m) - log((double)r.s));
       stats[row] = make_float2(none ? 0.f : r.m, none ? 0.f : 1.f / r.s);
     }
     __syncthreads();  // (s_part is read)

@@ -109,3 +109,20 @@ def test_a_margin_of_nan_logits_is_seen(S):
     ref = torch.tensor([0.0, float("nan"), 0.0, 0.0], device="cuda")
     loss, _, z = S.preference_loss(torch.zeros_like(x), t, ref)
     assert torch.isnan(loss) and torch.isnan(z[1])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_logprob_is_rounded_once(S, dtype):
+    """Rows whose sum of exponentials is exact: V - 1 equal logits, the label's so far below
+    that its own adds nothing.  The rest, difference and logarithm, is rounded once."""
+    import torch
+    g = gen(61)
+    for V in (2, 3, 10, 77, 1000, 4095, 50_001):
+        n = 600
+        top = normal(g, n, 1, dtype=dtype)
+        x = top.expand(n, V).clone()
+        x[:, -1] = (top[:, 0].float() - 120 - 40 * torch.rand(n, generator=g, device="cuda")).to(x.dtype)
+        t = torch.full((n,), V - 1, dtype=torch.int32, device="cuda")
+        X = R.f64(x)
+        want = (X[:, -1] - X[:, 0]) - np.log(V - 1)
+        near(S.label_logprob(x, t), want, R.U32 * np.abs(want) * (1 + 2.0 ** -20), f"{V} labels")
