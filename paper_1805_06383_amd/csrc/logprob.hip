@@ -24,8 +24,25 @@ namespace fstc {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eLow = 1.4426950408889634 - kLog2e;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBatch = 4;  // vectors a thread has in flight
+
+// e^x of x <= 0 by one rounded product: |x| 2^-24 of e^x off.  In a row's sum the
+// terms of weight have |x| of at most about log(vocab) on average, so the logarithm of the
+// sum is off by less than its own rounding; of a 16-bit gradient it is at most a hundredth of a unit.
+__device__ __forceinline__ float exp_below(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// The same for each element of a gradient.  In 32 bits a probability far below the row's largest
+// keeps its digits: 2^h (1 + l) with l what the rounded h lacks, three units of 2^-24 (those below
+// 2^-126 are 0).
+template <class T>
+__device__ __forceinline__ float exp_of(float x) {
+  if constexpr (!std::is_same<T, float>::value) return exp_below(x);
+  const float h = x * kLog2e, e = __builtin_amdgcn_exp2f(h);
+  const float l = fmaf(x, kLog2eLow * kLn2, fmaf(x, kLog2e, -h) * kLn2);
+  return e == 0.f ? e : fmaf(e, l, e);  // (x of -inf has no l)
+}
 
 // A running maximum and the sum of exp(x - maximum) of what was seen.
 struct MaxSum {
@@ -35,7 +52,7 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
   const float m = fmaxf(a.m, b.m);
   // (no -inf - -inf where nothing finite was seen)
   const float at = m == -INFINITY ? 0.f : m;
-  return {m, a.s * __builtin_amdgcn_exp2f((a.m - at) * kLog2e) + b.s * __builtin_amdgcn_exp2f((b.m - at) * kLog2e)};
+  return {m, a.s * exp_below(a.m - at) + b.s * exp_below(b.m - at)};
 }
 
 struct RowArgs {
@@ -73,12 +90,12 @@ __global__ __launch_bounds__(NT) void k_label_logprob(RowArgs a, const T *logits
 #pragma unroll
         for (int e = 0; e < N; ++e) m = fmaxf(m, to_f32(v[j].v[e]));
       const float at = m == -INFINITY ? 0.f : m;
-      float s = r.s * __builtin_amdgcn_exp2f((r.m - at) * kLog2e);
+      float s = r.s * exp_below(r.m - at);
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         float t = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) t += __builtin_amdgcn_exp2f((to_f32(v[j].v[e]) - at) * kLog2e);
+        for (int e = 0; e < N; ++e) t += exp_below(to_f32(v[j].v[e]) - at);
         s += c + j * NT < vectors ? t : 0.f;
       }
       r = {m, s};
@@ -117,7 +134,7 @@ __global__ __launch_bounds__(NT) void k_label_logprob_grad(RowArgs a, const T *l
     const bool zero = !live || st.y == 0.f;
     const float c = -w * st.y;
     auto grad = [&](float v, u32 at) {
-      const float p = c * __builtin_amdgcn_exp2f((v - st.x) * kLog2e);
+      const float p = c * exp_of<T>(v - st.x);
       return zero ? 0.f : at == (u32)y ? p + w : p;
     };
     // elements before the first 16-byte boundary of the output, whole pieces, the rest

@@ -126,3 +126,27 @@ def test_logprob_is_rounded_once(S, dtype):
         X = R.f64(x)
         want = (X[:, -1] - X[:, 0]) - np.log(V - 1)
         near(S.label_logprob(x, t), want, R.U32 * np.abs(want) * (1 + 2.0 ** -20), f"{V} labels")
+
+
+def test_float32_softmax_far_below_the_maximum(S):
+    """Probabilities of float32 logits 12 to 85 below the row's maximum, each to its own
+    digits.  The row's sum is 1 + at most 64 exp(-12): nine additions (four of a thread's elements,
+    one of its vectors, four of lanes) and its inverse, one unit of 2^-24 each, what the exponentials
+    below add is off by less than another; an exponential three, the product one."""
+    import torch
+    g = gen(62)
+    n, V = 700, 64
+    x = -12 - 73 * torch.rand(n, V, generator=g, device="cuda")
+    at = torch.randint(0, V, (n,), generator=g, device="cuda")
+    shift = normal(g, n, scale=3.0)
+    x[torch.arange(n), at] = 0
+    # (differences from the maximum without a rounding)
+    x = torch.round((x + shift[:, None]) * 2.0 ** 16) / 2.0 ** 16
+    x.requires_grad_()
+    d, = torch.autograd.grad(S.label_logprob(x, at), x, torch.ones(n, device="cuda"))
+    X = R.f64(x)
+    want = -R.logprob(X, at.cpu().numpy())[1]
+    others = np.ones((n, V), bool)
+    others[np.arange(n), at.cpu().numpy()] = False
+    off = np.abs(R.f64(d) / want - 1)[others]
+    assert off.max() <= 15 * R.U32, f"{off.max() / R.U32:.1f} units"
