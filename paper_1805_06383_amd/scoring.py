@@ -261,8 +261,8 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0, parents
     (parents int32 [batch]; one outside [0, rows), such as -1, starts from a zero
     state), or from state[b] without parents (rows = batch).  Returns (out
     [batch, heads, dim_v], new states [batch, heads, dim_k, dim_v]).  out_state
-    receives the new states; it may be `state` itself when there are no
-    parents.  Not differentiable (train with linear_attention)."""
+    receives the new states, as an in-place operation does; it may be `state` itself
+    when there are no parents.  Not differentiable (train with linear_attention)."""
     q, k, v, log_decay = _attention_inputs(q, k, v, log_decay, 3)
     B, H, dk = q.shape
     dv = v.shape[2]
@@ -276,16 +276,24 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0, parents
             _refuse(f"parents: int32 ({B},) on {q.device}, not {parents.dtype} "
                     f"{tuple(parents.shape)} on {parents.device}")
         parents = parents.contiguous()
+    versioned = False
     if out_state is None:
         out_state = state.new_empty((B, H, dk, dv))
-    elif not out_state.is_contiguous() or _f32("out_state", out_state, (B, H, dk, dv), q) is None:
-        _refuse("out_state has to be contiguous")
+    else:
+        if not out_state.is_contiguous():
+            _refuse("out_state has to be contiguous")
+        _f32("out_state", out_state, (B, H, dk, dv), q)
+        if out_state.requires_grad and torch.is_grad_enabled():
+            _refuse("out_state wants a gradient, which a step does not have: call it under torch.no_grad()")
+        versioned = not out_state.is_inference()
     out = q.new_empty((B, H, dv))
     (qb, qh, _), (kb, kh, _), (vb, vh, _) = q.stride(), k.stride(), v.stride()
     args = _linattn_args((B, 1, H, dk), dv, q.dtype, log_decay, scale, state, None, q, k, v,
                          (qb, 0, qh), (kb, 0, kh), (vb, 0, vh))
     _call("fstc_linattn_step", q.device, args, parents.data_ptr() if parents is not None else None,
           rows, out_state.data_ptr(), out.data_ptr())
+    if versioned:  # (a backward pass that has kept it must not use it as it is now)
+        torch.autograd.graph.increment_version(out_state)
     return out, out_state
 
 

@@ -150,3 +150,46 @@ def test_float32_softmax_far_below_the_maximum(S):
     others[np.arange(n), at.cpu().numpy()] = False
     off = np.abs(R.f64(d) / want - 1)[others]
     assert off.max() <= 15 * R.U32, f"{off.max() / R.U32:.1f} units"
+
+
+def test_step_in_place_is_seen_by_autograd(S):
+    """A state that a step writes while a backward pass still needs it: the pass raises, as
+    after any in-place operation."""
+    import torch
+    g = gen(63)
+    q, k, v = (normal(g, 2, 5, 2, 8).requires_grad_() for _ in range(3))
+    one = [normal(g, 2, 2, 8) for _ in range(3)]
+    ld = -torch.rand(2, generator=g, device="cuda")
+    pool = normal(g, 4, 2, 8, 8)
+    parents = torch.tensor([3, 2], dtype=torch.int32, device="cuda")
+    for args, out_state in ((dict(state=pool[:2]), pool[:2]),
+                            (dict(state=pool[2:].clone(), parents=parents - 2), pool[:2])):
+        out, _ = S.linear_attention(q, k, v, ld, initial_state=pool[:2])
+        torch.autograd.grad(out.sum(), q, retain_graph=True)
+        S.linear_attention_step(*one, ld, out_state=out_state, **args)
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            torch.autograd.grad(out.sum(), q)
+    # written by a step without the caller's buffer: nothing changes under the pass
+    out, _ = S.linear_attention(q, k, v, ld, initial_state=pool[:2])
+    S.linear_attention_step(*one, ld, pool[:2])
+    torch.autograd.grad(out.sum(), q)
+    with torch.inference_mode():
+        state = torch.ones(2, 2, 8, 8, device="cuda")
+        o, new = S.linear_attention_step(*one, ld, state, out_state=state)
+        assert new is state and torch.isfinite(o).all()
+
+
+def test_step_into_a_state_that_wants_a_gradient(S):
+    import torch
+    from paper_1805_06383_amd.fstc import FstcError
+    g = gen(64)
+    one = [normal(g, 2, 2, 8) for _ in range(3)]
+    ld = torch.zeros(2, device="cuda")
+    state = normal(g, 2, 2, 8, 8)
+    leaf = torch.zeros_like(state).requires_grad_()
+    with pytest.raises(FstcError, match="gradient"):
+        S.linear_attention_step(*one, ld, state, out_state=leaf)
+    assert not leaf.any()
+    with torch.no_grad():
+        S.linear_attention_step(*one, ld, state, out_state=leaf)
+    assert leaf.any()
