@@ -17,7 +17,8 @@ Tensors are float32, bfloat16 or float16 on one GPU; labels are int32 (the
 bits of the u32 labels of a transducer) or int64, and a label outside its
 alphabet, such as -1, marks padding.  Work is enqueued on the current stream of
 the tensors' device.  Arguments that an operator does not take raise
-``FstcError`` before anything is enqueued.
+``FstcError`` before anything is enqueued, and so do derivatives that it does not have
+(second ones, those of forward mode).
 """
 from __future__ import annotations
 
@@ -25,6 +26,7 @@ import ctypes
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from .fstc import (FSTC_ERR_INVALID_ARG, FstcError, FstcLinattnArgs, _check, load_library)
 
@@ -85,10 +87,22 @@ def _call(name: str, device: torch.device, *args):
         _check(rc)
 
 
-def _first_derivatives_only():
+def _refuse_lost(*tensors):
+    """Refuses what would lose an operator without a word: a tangent of forward-mode
+    differentiation, and a trace, which records allocations and no kernel."""
+    if forward_ad._current_level >= 0:
+        for x in tensors:
+            if x is not None and forward_ad.unpack_dual(x).tangent is not None:
+                _refuse("forward-mode derivatives are not available")
+    if torch.jit.is_tracing():
+        _refuse("the operators cannot be traced")
+
+
+def _first_derivatives_only(*grads):
     # (a backward pass runs with gradients enabled where it is to be differentiated itself)
     if torch.is_grad_enabled():
         _refuse("second derivatives are not available")
+    _refuse_lost(*grads)
 
 
 def _workspace(nbytes: int, like: torch.Tensor):
@@ -117,7 +131,7 @@ class _Embed(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        _first_derivatives_only()
+        _first_derivatives_only(grad)
         (labels,) = ctx.saved_tensors
         (rows, dim), n = ctx.shape, labels.numel()
         grad = _rows(grad.reshape(n, dim))
@@ -136,6 +150,7 @@ def embed(table: torch.Tensor, labels: torch.Tensor, scale: float = 1.0) -> torc
     """scale * table[labels]: [*labels.shape, dim] of the table's type; zero
     rows for labels outside [0, len(table)).  Differentiable in the table; the
     gradient's sums have a fixed order (equal inputs give equal bits)."""
+    _refuse_lost(table)
     _values("table", table, 2)
     table = _rows(table)
     if table.shape[0] > 1 and table.stride(0) < table.shape[1]:
@@ -189,7 +204,7 @@ class _LinearAttention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dout, dfinal):
-        _first_derivatives_only()
+        _first_derivatives_only(dout, dfinal)
         q, k, v, log_decay, init, lengths = ctx.saved_tensors
         if dout is None:
             dout = torch.zeros((), dtype=q.dtype, device=q.device).expand(*q.shape[:3], v.shape[3])
@@ -237,6 +252,7 @@ def linear_attention(q, k, v, log_decay, scale: float = 1.0, initial_state=None,
     final_state): out has q's type, zero at and beyond a row's length;
     final_state is float32, the state after the row's last position, from which
     linear_attention_step goes on.  Differentiable in q, k, v and initial_state."""
+    _refuse_lost(q, k, v, log_decay, initial_state)
     q, k, v, log_decay = _attention_inputs(q, k, v, log_decay, 4)
     B, T, H, dk = q.shape
     if initial_state is not None:
@@ -263,6 +279,7 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0, parents
     [batch, heads, dim_v], new states [batch, heads, dim_k, dim_v]).  out_state
     receives the new states, as an in-place operation does; it may be `state` itself
     when there are no parents.  Not differentiable (train with linear_attention)."""
+    _refuse_lost(q, k, v, log_decay, state, out_state)
     q, k, v, log_decay = _attention_inputs(q, k, v, log_decay, 3)
     B, H, dk = q.shape
     dv = v.shape[2]
@@ -340,7 +357,7 @@ class _LabelLogprob(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        _first_derivatives_only()
+        _first_derivatives_only(grad)
         x, labels, kept = ctx.saved_tensors
         grad = grad.contiguous()
         return _logprob_grad(ctx.shape, x, *ctx.rows, labels, ctx.size, kept, grad.data_ptr(), 1,
@@ -353,6 +370,7 @@ def label_logprob(logits: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
     vocabulary.  Logits may be -inf (labels that a transducer does not allow);
     a row of nothing else has log-probability -inf and a zero gradient.
     Differentiable in the logits."""
+    _refuse_lost(logits)
     if tuple(logits.shape[:-1]) != tuple(labels.shape):
         _refuse(f"logits {tuple(logits.shape)} for labels {tuple(labels.shape)}")
     _values("logits", logits, logits.ndim)
@@ -388,7 +406,7 @@ class _Preference(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad, _seq, _margin):
-        _first_derivatives_only()
+        _first_derivatives_only(grad)
         x, labels, kept = ctx.saved_tensors
         return _logprob_grad(ctx.shape, x, *ctx.rows, labels, ctx.size, kept,
                              kept.data_ptr() + 8 * ctx.rows[0], max(1, labels.shape[1]),
@@ -411,6 +429,7 @@ def preference_loss(logits: torch.Tensor, labels: torch.Tensor, ref_logprob: tor
     (both sequences of a pair, or a sequence and its reference) the margin is NaN
     and the pair adds nothing to the loss or its gradient.  The loss is
     differentiable in the logits; logprob and margin are for reading."""
+    _refuse_lost(logits, ref_logprob)
     if labels.ndim != 2 or labels.shape[0] % 2 or labels.shape[0] == 0:
         _refuse(f"labels: [2 * pairs, length], not {tuple(labels.shape)}")
     if tuple(logits.shape[:-1]) != tuple(labels.shape):

@@ -193,3 +193,51 @@ def test_step_into_a_state_that_wants_a_gradient(S):
     with torch.no_grad():
         S.linear_attention_step(*one, ld, state, out_state=leaf)
     assert leaf.any()
+
+
+def calls_of(S):
+    """(name, function of its floating inputs, the inputs) of each operator."""
+    import torch
+    g = gen(65)
+    t = torch.tensor([[1, 2], [3, 0]], dtype=torch.int32, device="cuda")
+    ld = -torch.rand(2, generator=g, device="cuda")
+    q = [normal(g, 2, 3, 2, 4) for _ in range(3)]
+    one = [normal(g, 2, 2, 4) for _ in range(3)]
+    s0 = normal(g, 2, 2, 4, 4)
+    x = normal(g, 2, 2, 5)
+    ref = normal(g, 2)
+    return [("embed", lambda w: S.embed(w, t), [normal(g, 5, 4)]),
+            ("linear_attention", lambda *a: S.linear_attention(*a[:4], initial_state=a[4]), [*q, ld, s0]),
+            ("linear_attention_step", lambda *a: S.linear_attention_step(*a), [*one, ld, s0]),
+            ("label_logprob", lambda y: S.label_logprob(y, t), [x]),
+            ("preference_loss", lambda y, r: S.preference_loss(y, t, r), [x, ref])]
+
+
+def test_forward_mode_derivatives_are_refused(S):
+    import torch
+    import torch.autograd.forward_ad as fwd
+    from paper_1805_06383_amd.fstc import FstcError
+    for name, f, inputs in calls_of(S):
+        for i in range(len(inputs)):
+            with fwd.dual_level():
+                f(*inputs)  # (no tangents: as ever)
+                dual = list(inputs)
+                dual[i] = fwd.make_dual(inputs[i], torch.ones_like(inputs[i]))
+                with pytest.raises(FstcError, match="forward-mode"):
+                    f(*dual)
+            if name == "linear_attention_step":
+                continue
+            # the tangent of what a backward pass starts from
+            y = f(inputs[0].clone().requires_grad_(), *inputs[1:])
+            y = y if isinstance(y, torch.Tensor) else y[0]
+            with fwd.dual_level(), pytest.raises(FstcError, match="forward-mode"):
+                y.backward(fwd.make_dual(torch.ones_like(y), torch.ones_like(y)))
+
+
+def test_tracing_is_refused(S):
+    import torch
+    from paper_1805_06383_amd.fstc import FstcError
+    for name, f, inputs in calls_of(S):
+        with pytest.raises(FstcError, match="trace"):
+            torch.jit.trace(f, tuple(inputs), check_trace=False)
+        f(*inputs)
