@@ -18,7 +18,7 @@ bits of the u32 labels of a transducer) or int64, and a label outside its
 alphabet, such as -1, marks padding.  Work is enqueued on the current stream of
 the tensors' device.  Arguments that an operator does not take raise
 ``FstcError`` before anything is enqueued, and so do derivatives that it does not have
-(second ones, those of forward mode).
+(second ones, those of forward mode, those in a decay or a reference).
 """
 from __future__ import annotations
 
@@ -420,7 +420,8 @@ def preference_loss(logits: torch.Tensor, labels: torch.Tensor, ref_logprob: tor
     logits [2 * pairs, length, vocab], labels [2 * pairs, length] (padding:
     labels outside the vocabulary): sequence p of the first half is preferred to
     sequence pairs + p.  ref_logprob float32 [2 * pairs]: the sequences'
-    log-probabilities under a reference model (sums of label_logprob).  Returns
+    log-probabilities under a reference model (sums of label_logprob), which is fixed
+    (no gradient).  Returns
     (loss, logprob [2 * pairs], margin [pairs]), float32: with L the sequences'
     log-probabilities, margin = beta * ((L - ref) of the preferred - (L - ref) of
     the other), loss = mean of -(1 - label_smoothing) log sigmoid(margin) -
@@ -436,7 +437,9 @@ def preference_loss(logits: torch.Tensor, labels: torch.Tensor, ref_logprob: tor
         _refuse(f"logits {tuple(logits.shape)} for labels {tuple(labels.shape)}")
     _values("logits", logits, 3)
     labels, size = _labels("labels", labels, logits)
-    ref = _f32("ref_logprob", ref_logprob, labels.shape[:1], logits).detach()
+    if ref_logprob.requires_grad and torch.is_grad_enabled():
+        _refuse("ref_logprob is of a fixed model: it has no gradient (pass it detached)")
+    ref = _f32("ref_logprob", ref_logprob, labels.shape[:1], logits)
     if logits.requires_grad and torch.is_grad_enabled():
         return _Preference.apply(logits, labels, size, ref, float(beta), float(label_smoothing))
     return _preference_forward(*_logit_rows(logits), labels, size, ref, float(beta),

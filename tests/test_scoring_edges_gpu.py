@@ -241,3 +241,17 @@ def test_tracing_is_refused(S):
         with pytest.raises(FstcError, match="trace"):
             torch.jit.trace(f, tuple(inputs), check_trace=False)
         f(*inputs)
+
+
+def test_a_reference_that_wants_a_gradient_is_refused(S):
+    import torch
+    from paper_1805_06383_amd.fstc import FstcError
+    x = torch.zeros(2, 3, 5, device="cuda", requires_grad=True)
+    t = torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    ref = torch.zeros(2, device="cuda", requires_grad=True)
+    for y in (x, x.detach()):
+        with pytest.raises(FstcError, match="ref_logprob"):
+            S.preference_loss(y, t, ref)
+    S.preference_loss(x, t, ref.detach())[0].backward()
+    with torch.no_grad():
+        S.preference_loss(x, t, ref)
