@@ -436,6 +436,8 @@ def preference_loss(logits: torch.Tensor, labels: torch.Tensor, ref_logprob: tor
     if tuple(logits.shape[:-1]) != tuple(labels.shape):
         _refuse(f"logits {tuple(logits.shape)} for labels {tuple(labels.shape)}")
     _values("logits", logits, 3)
+    if not 0 <= ctypes.c_float(label_smoothing).value < 0.5:  # (as the call rounds it)
+        _refuse(f"label_smoothing has to be in [0, 0.5), not {label_smoothing}")
     labels, size = _labels("labels", labels, logits)
     if ref_logprob.requires_grad and torch.is_grad_enabled():
         _refuse("ref_logprob is of a fixed model: it has no gradient (pass it detached)")

@@ -255,3 +255,20 @@ def test_a_reference_that_wants_a_gradient_is_refused(S):
     S.preference_loss(x, t, ref.detach())[0].backward()
     with torch.no_grad():
         S.preference_loss(x, t, ref)
+
+
+def test_preference_loss_refuses_before_it_enqueues(S, monkeypatch):
+    import torch
+    from paper_1805_06383_amd.fstc import FstcError
+    x = torch.zeros(2, 3, 5, device="cuda")
+    t = torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    ref = torch.zeros(2, device="cuda")
+    called, call = [], S._call
+    monkeypatch.setattr(S, "_call", lambda name, *a: (called.append(name), call(name, *a))[1])
+    for eps in (0.5, -0.1, float("nan")):
+        for y in (x, x.clone().requires_grad_()):
+            with pytest.raises(FstcError, match="label_smoothing"):
+                S.preference_loss(y, t, ref, label_smoothing=eps)
+    assert not called
+    S.preference_loss(x, t, ref, label_smoothing=0.49)
+    assert called
