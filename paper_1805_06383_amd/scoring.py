@@ -28,7 +28,8 @@ import struct
 import torch
 from torch.autograd import forward_ad
 
-from .fstc import (FSTC_ERR_INVALID_ARG, FstcError, FstcLinattnArgs, _check, load_library)
+from .fstc import (FSTC_ERR_INVALID_ARG, FSTC_ERR_RANGE, FstcError, FstcLinattnArgs, _check,
+                   load_library)
 
 __all__ = ["embed", "label_logprob", "linear_attention", "linear_attention_step",
            "preference_loss"]
@@ -159,6 +160,8 @@ def embed(table: torch.Tensor, labels: torch.Tensor, scale: float = 1.0) -> torc
         table = table.as_strided(table.shape, (table.shape[1], 1))
     labels, size = _labels("labels", labels, table)
     if table.requires_grad and torch.is_grad_enabled():
+        if max(table.shape[0], labels.numel()) >= 1 << 28:
+            raise FstcError(FSTC_ERR_RANGE, "rows and labels must be below 2^28 for the gradient")
         return _Embed.apply(table, labels, size, float(scale))
     return _embed_forward(table, labels, size, float(scale))
 

@@ -272,3 +272,19 @@ def test_preference_loss_refuses_before_it_enqueues(S, monkeypatch):
     assert not called
     S.preference_loss(x, t, ref, label_smoothing=0.49)
     assert called
+
+
+def test_embed_refuses_what_its_gradient_would(S):
+    """A table of 2^28 rows has a lookup but no gradient: asked for one, the lookup refuses."""
+    import torch
+    from paper_1805_06383_amd.fstc import FSTC_ERR_RANGE, FstcError
+    w = torch.zeros(1 << 28, 1, dtype=torch.bfloat16, device="cuda")
+    t = torch.tensor([0, (1 << 28) - 1], dtype=torch.int64, device="cuda")
+    w[-1] = 3.0
+    assert S.embed(w, t).tolist() == [[0.0], [3.0]]
+    w.requires_grad_()
+    with pytest.raises(FstcError, match="2\\^28") as e:
+        S.embed(w, t)
+    assert e.value.code == FSTC_ERR_RANGE
+    with torch.no_grad():
+        S.embed(w, t)
