@@ -458,8 +458,8 @@ int fstc_linattn_grad(const fstc_linattn_args *args, const void *dout, const int
 /*
  * fstc_linattn_step: one position for each row (args->length 1, no lengths):
  * row b continues from the state init[parents[b]] (init [state_rows, heads,
- * dim_k, dim_v]; a parent outside it: from a zero state), so that a hypothesis
- * can be continued by several labels.  parents NULL: row b continues init[b]
+ * dim_k, dim_v]; a parent outside it: from a zero state; state_rows may be 0),
+ * so that a hypothesis can be continued by several labels.  parents NULL: row b continues init[b]
  * (state_rows = batch).
  *   state   [batch, heads, dim_k, dim_v] receives the states; it may be init
  *           itself when parents is NULL, and must not overlap it otherwise

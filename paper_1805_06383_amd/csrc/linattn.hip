@@ -788,7 +788,7 @@ int fstc_linattn_step(const fstc_linattn_args *args, const int32_t *parents, uin
   if (args->length != 1) return report_failure(FSTC_ERR_INVALID_ARG, "a step has length 1");
   if (args->lengths) return report_failure(FSTC_ERR_INVALID_ARG, "a step takes no lengths");
   if (args->batch == 0) return FSTC_OK;
-  if (!args->init || !state || !out)
+  if ((state_rows && !args->init) || !state || !out)
     return report_failure(FSTC_ERR_INVALID_ARG, "init, state or out is NULL");
   if (state_rows >= (1u << 31)) return report_failure(FSTC_ERR_RANGE, "state_rows must be below 2^31");
   const u64 row = (u64)args->heads * args->dim_k * args->dim_v * sizeof(float);

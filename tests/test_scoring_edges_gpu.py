@@ -288,3 +288,15 @@ def test_embed_refuses_what_its_gradient_would(S):
     assert e.value.code == FSTC_ERR_RANGE
     with torch.no_grad():
         S.embed(w, t)
+
+
+def test_step_from_no_states(S):
+    """Hypotheses that all start anew, and a pool of no states."""
+    import torch
+    g = gen(66)
+    one = [normal(g, 3, 2, 8) for _ in range(3)]
+    ld = -torch.rand(2, generator=g, device="cuda")
+    fresh = torch.full((3,), -1, dtype=torch.int32, device="cuda")
+    out, new = S.linear_attention_step(*one, ld, torch.empty(0, 2, 8, 8, device="cuda"), parents=fresh)
+    want, state = S.linear_attention_step(*one, ld, torch.ones(1, 2, 8, 8, device="cuda"), parents=fresh)
+    assert torch.equal(out, want) and torch.equal(new, state)
