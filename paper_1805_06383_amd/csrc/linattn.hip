@@ -272,7 +272,8 @@ struct JoinArgs {
 struct JoinJobs {
   JoinArgs j[2];
   u32 segments, segment, rows, cols, A, W;
-  u32 heads, length, blocks_per;
+  u32 heads, length, blocks_per;  // workgroups' parts of a batch row's head, and of all
+  u32 blocks;
   const float *log_decay;
   const int32_t *lengths;
 };
@@ -286,34 +287,39 @@ __device__ __forceinline__ float2 segment_decays(const JoinJobs &a, u32 h, u32 l
 }
 
 // A thread an element: kFew segments' are on their way before the first is added.
+// (One segment of padded states may have 2^20 states of 256 workgroups' parts: more threads than a
+// launch holds, so the parts are walked by the grid.)
 constexpr u32 kFew = 8;
 __global__ __launch_bounds__(kNT) void k_join_few(JoinJobs a) {
   const JoinArgs &job = a.j[blockIdx.y];
-  const u32 bh = blockIdx.x / a.blocks_per, cells = a.rows * a.cols;
-  const u32 i = blockIdx.x % a.blocks_per * kNT + threadIdx.x;
-  const u32 len = row_length(a.lengths, bh / a.heads, a.length);
-  const float2 decay = segment_decays(a, bh % a.heads, len);
-  const float whole = decay.x, last = decay.y;
-  if (i >= cells) return;
-  const u32 ka = i / a.cols, w = i % a.cols;
-  const bool in = ka < a.A && w < a.W;
-  const u64 outside = (u64)bh * a.A * a.W + ka * a.W + w;
-  float s = in && job.init ? job.init[outside] : 0.f;
-  float *p = job.state + (u64)bh * a.segments * cells + i;
-  for (u32 k0 = 0; k0 < a.segments; k0 += kFew) {
-    float own[kFew];
+  for (u32 block = blockIdx.x; block < a.blocks; block += gridDim.x) {
+    const u32 bh = block / a.blocks_per, cells = a.rows * a.cols;
+    const u32 i = block % a.blocks_per * kNT + threadIdx.x;
+    const u32 len = row_length(a.lengths, bh / a.heads, a.length);
+    const float2 decay = segment_decays(a, bh % a.heads, len);
+    const float whole = decay.x, last = decay.y;
+    __syncthreads();  // (the next part's decays go where these were)
+    if (i >= cells) continue;
+    const u32 ka = i / a.cols, w = i % a.cols;
+    const bool in = ka < a.A && w < a.W;
+    const u64 outside = (u64)bh * a.A * a.W + ka * a.W + w;
+    float s = in && job.init ? job.init[outside] : 0.f;
+    float *p = job.state + (u64)bh * a.segments * cells + i;
+    for (u32 k0 = 0; k0 < a.segments; k0 += kFew) {
+      float own[kFew];
 #pragma unroll
-    for (u32 j = 0; j < kFew; ++j) own[j] = p[(u64)min(k0 + j, a.segments - 1) * cells];
+      for (u32 j = 0; j < kFew; ++j) own[j] = p[(u64)min(k0 + j, a.segments - 1) * cells];
 #pragma unroll
-    for (u32 j = 0; j < kFew; ++j) {
-      const u32 k = k0 + j;
-      if (k >= a.segments) break;
-      p[(u64)k * cells] = s;
-      const u32 ends = len / a.segment;
-      s = fmaf(k < ends ? whole : k == ends ? last : 1.f, s, own[j]);
+      for (u32 j = 0; j < kFew; ++j) {
+        const u32 k = k0 + j;
+        if (k >= a.segments) break;
+        p[(u64)k * cells] = s;
+        const u32 ends = len / a.segment;
+        s = fmaf(k < ends ? whole : k == ends ? last : 1.f, s, own[j]);
+      }
     }
+    if (in && job.final) job.final[outside] = s;
   }
-  if (in && job.final) job.final[outside] = s;
 }
 
 // Of many segments: a workgroup owns 64 elements, and its waves take kAhead segments
@@ -621,7 +627,9 @@ void join_segments(const fstc_linattn_args &a, const Plan &pl, const JoinArgs *j
   r.lengths = a.lengths;
   const bool many = pl.segments > kMany;
   r.blocks_per = (u32)ceil_div(pl.rows * pl.cols, many ? kWave : kNT);
-  const dim3 grid(a.batch * a.heads * r.blocks_per, n);
+  r.blocks = a.batch * a.heads * r.blocks_per;  // below 2^28
+  // (k_join_many does not walk: where there are many segments, there are fewer states than kMostGroups)
+  const dim3 grid(std::min<u32>(r.blocks, (u32)kMaxGrid), n);
   if (many) hipLaunchKernelGGL(k_join_many, grid, dim3(kNT), 0, s, r);
   else hipLaunchKernelGGL(k_join_few, grid, dim3(kNT), 0, s, r);
 }

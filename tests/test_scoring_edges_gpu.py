@@ -300,3 +300,21 @@ def test_step_from_no_states(S):
     out, new = S.linear_attention_step(*one, ld, torch.empty(0, 2, 8, 8, device="cuda"), parents=fresh)
     want, state = S.linear_attention_step(*one, ld, torch.ones(1, 2, 8, 8, device="cuda"), parents=fresh)
     assert torch.equal(out, want) and torch.equal(new, state)
+
+
+def test_attention_of_many_short_rows(S):
+    """65,536 states, padded to 256 x 256: their join, a thread an element, would be more threads
+    than one launch holds.  Every batch row repeats one of four, by bits."""
+    import torch
+    g = gen(67)
+    B, H, T, dk, dv, few = 4096, 16, 2, 130, 132, 4
+    q, k = (normal(g, few, T, H, dk, dtype="bfloat16") for _ in range(2))
+    v = normal(g, few, T, H, dv, dtype="bfloat16")
+    ld = -torch.rand(H, generator=g, device="cuda")
+    s0 = normal(g, few, H, dk, dv)
+    many = [x.repeat(B // few, *[1] * (x.ndim - 1)) for x in (q, k, v)]
+    s1 = s0.repeat(B // few, 1, 1, 1)
+    out, final = S.linear_attention(q, k, v, ld, initial_state=s0)
+    o, f = S.linear_attention(*many, ld, initial_state=s1)
+    assert torch.equal(o.view(-1, *out.shape), out.expand(B // few, *out.shape))
+    assert torch.equal(f.view(-1, *final.shape), final.expand(B // few, *final.shape))
