@@ -12,12 +12,12 @@
 // loops that need not be unrolled are not: the first chunk of a launch waits for its
 // instructions too (0.5 us a KB of them).
 //
-// Measured: 100,003 positions of 8 heads, 64 x 64 states, 83 us for 410 MB
-// (4.9 TB/s, the rate of a large copy) after 42 us of segment states; 4 x 4,096
-// positions of 16 heads, 128 x 128 states, 67 us for 268 MB in four segments, and
-// 228 to 265 us for the three gradients in one segment, 192 workgroups of which
-// each has a compute unit to itself: 3.8 us a chunk, of which the vector, the
-// matrix and the LDS units are busy 56%, 38% and 52%, in turn.
+// Measured: 100,003 positions of 8 heads, 64 x 64 states, 92 us for 410 MB
+// (4.5 TB/s) after 41 us of segment states; 4 x 4,096 positions of 16 heads, 128 x 128
+// states, 85 us for 268 MB in eight segments, and 290 to 335 us for the three gradients
+// in one segment, 192 workgroups of which each has a compute unit to itself:
+// 4.3 us a chunk, of which the vector, the matrix and the LDS units are busy 68%, 42%
+// and 42%, in turn.
 //
 // A lane's eight elements of a contraction are those that a result gives it
 // (32 x 32: rows 4 h + r and 8 + 4 h + r of each 16, h = lane / 32).  The
@@ -26,18 +26,18 @@
 // and each gets its column of them.
 //
 // q.k products of 16-bit factors are exact in the matrix unit.  The other
-// products have one 32-bit factor, taken in 16-bit parts: the scores and the
-// state (for the outputs, which are rounded to 8 significant bits anyway) in
-// two, which keeps 16 bits; the weighted values (for the state, which is held
-// and returned in 32 bits) in three, which keeps 24.  What is left of an infinity is
+// products have one 32-bit factor (the scores, the entering state, the weighted
+// values), taken in three 16-bit parts, which keep its 24 bits: a state of 2^23 and
+// one of a unit less still differ by that unit in an output.  (Two parts, 16 bits, would
+// do for outputs that do not cancel, in four fifths of the time.)  What is left of an infinity is
 // NaN: an infinite input, score or state gives NaN where the sum would be infinite.
 //
 // A float16 input is taken apart into two bfloat16 parts as it enters LDS, which is
-// exact (8 and 3 bits), and products of two low parts are left out (2^-16 of a
-// term; of the returned state 2^-24): bfloat16's range, whatever the states
-// and scores grow to.  It costs half as many products again and twice the LDS,
-// so dimensions to 128; 4 x 4,096 positions of 16 heads, 128 x 128: forward and
-// gradients in 471 us, 1,360 on the 32-bit instructions.
+// exact (8 and 3 bits): bfloat16's range, whatever the states and scores grow to.  Of
+// a 32-bit factor the lowest part times an input's low one is left out (2^-25 of a
+// term).  It costs two thirds as many products again (of the scores four times as many) and
+// twice the LDS, so dimensions to 128; 4 x 4,096 positions of 16 heads, 128 x 128: forward and
+// gradients in 610 us, 1,360 on the 32-bit instructions.
 #include "linattn.hpp"
 
 namespace fstc {
@@ -50,9 +50,6 @@ using s16x4 = short __attribute__((ext_vector_type(4)));
 using f32x2 = float __attribute__((ext_vector_type(2)));
 using f32x16 = float __attribute__((ext_vector_type(16)));
 
-__device__ __forceinline__ f32x4 mfma16(b16x8 a, b16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
 __device__ __forceinline__ f32x16 mfma32(b16x8 a, b16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -113,6 +110,18 @@ __device__ __forceinline__ auto as_vector(const bf16 (&x)[N]) {
 #pragma unroll
   for (int e = 0; e < N; ++e) y[e] = x[e];
   return y;
+}
+
+// A number in 16-bit parts, which sum to it but for what N of them cannot hold.
+template <int N>
+__device__ __forceinline__ void parts_of(float (&x)[8], b16x8 (&part)[N]) {
+#pragma unroll
+  for (int i = 0; i < N - 1; ++i) {
+    bf16 y[8];
+    take_part(x, y);
+    part[i] = as_vector(y);
+  }
+  part[N - 1] = round_all(x);
 }
 
 // Eight 16-bit elements without the first n, which may be 8 and more; zeros follow.
@@ -235,22 +244,23 @@ __device__ __forceinline__ void move_state(f32x16 (&st)[AB], float *p, const Sta
 // AB: blocks of 32 that hold the contraction's A elements; NW: blocks of 32 columns.
 // P: waves of a block of columns, each with its share of the state's rows.  Of
 // two, each forms its rows' part of all 64 outputs, hands the other 32 queries'
-// to its partner through LDS, and finishes its own 32.  EXACT: the state after a
-// segment is wanted.
+// to its partner through LDS, and finishes its own 32.
 constexpr u32 kNone = 32;  // keys after the query, at most 31 in a block of 32
-template <class T, int AB, int NW, int P, bool OUT, bool EXACT, bool FAST>
+constexpr int kParts = 3;   // 16-bit parts of a 32-bit factor
+template <class T, int AB, int NW, int P, bool OUT, bool FAST>
 __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(AttendJobs jobs) {
   // Rows of the tiles are kPad elements apart more: 24 halve the bank conflicts of 8
-  // (3.7 -> 3.5 us a chunk of 128 x 128 states); of 64 x 64 states four workgroups
-  // share a compute unit's LDS with 8, three with 24 (6.5, 6.9 us a chunk).
+  // (15.8 for 16.0 us a chunk of four workgroups of 128 x 128 states); of 64 x 64 states four
+  // workgroups share a compute unit's LDS with 8, three with 24 (6.2, 8.9 us).
   constexpr int kPad = AB == 2 && NW == 2 ? 8 : 24;
   constexpr int SB = AB / P, kThreads = P * NW * kWave, kTile = NW * 32, kA = AB * 32, kLdA = kA + kPad, kLdV = kTile + kPad;
-  constexpr int kParts = EXACT ? 3 : 2;  // of a weighted value
   constexpr int kIn = std::is_same<T, bf16>::value ? 1 : 2;  // of an input
   constexpr int kPlaneA = kChunk16 * kLdA, kPlaneV = kChunk16 * kLdV;
   __shared__ __align__(16) bf16 s_q[OUT ? kIn * kPlaneA : 8], s_k[kIn * kPlaneA], s_v[kIn * kPlaneV];
   // scores as operands of 32 queries: key blocks 0 and 1 of the first 32, 0 to 3 of the others
-  __shared__ __align__(16) bf16 s_p[2][OUT ? 6 * kWave * 8 : 8];
+  // (32 bits a score, which each wave takes apart: three parts would be 6 bytes, and leave room
+  // for three workgroups of 64 x 64 states on a compute unit, not four: 8.0 us a chunk, not 6.2)
+  __shared__ __align__(16) float s_p[OUT ? 6 * kWave * 8 : 8];
   __shared__ f32x4 s_part[P == 2 ? P * NW * 4 * kWave : 1];  // outputs for the partner
   __shared__ float s_pow[kChunk16 + 1];                // g^n
   __shared__ float s_factor[OUT ? kNone + kChunk16 : 1];  // of a score, by query - key + kNone
@@ -333,8 +343,11 @@ __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(At
           const b16x8 x0 = *reinterpret_cast<const b16x8 *>(sk + m * 16), y0 = *reinterpret_cast<const b16x8 *>(sq + m * 16);
           p = mfma32(x0, y0, p);
           if constexpr (kIn == 2) {
-            p = mfma32(*reinterpret_cast<const b16x8 *>(sk + kPlaneA + m * 16), y0, p);
-            p = mfma32(x0, *reinterpret_cast<const b16x8 *>(sq + kPlaneA + m * 16), p);
+            const b16x8 x1 = *reinterpret_cast<const b16x8 *>(sk + kPlaneA + m * 16);
+            p = mfma32(x1, y0, p);
+            const b16x8 y1 = *reinterpret_cast<const b16x8 *>(sq + kPlaneA + m * 16);
+            p = mfma32(x0, y1, p);
+            p = mfma32(x1, y1, p);
           }
         }
         // query l32, key 8 (r / 4) + 4 half + r % 4: decayed, 0 for keys after the query
@@ -344,11 +357,9 @@ __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(At
         for (int r = 0; r < 16; ++r) z[r / 8][r % 8] = p[r] * f[27 - r / 4 * 8 - r % 4];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          bf16 hi[8];
-          take_part(z[y], hi);
           const u32 at = ((it * 2 + jt * 2 + y) * kWave + lane) * 8;
-          *reinterpret_cast<b16x8 *>(s_p[0] + at) = as_vector(hi);
-          *reinterpret_cast<b16x8 *>(s_p[1] + at) = round_all(z[y]);
+          *reinterpret_cast<f32x4 *>(s_p + at) = f32x4{z[y][0], z[y][1], z[y][2], z[y][3]};
+          *reinterpret_cast<f32x4 *>(s_p + at + 4) = f32x4{z[y][4], z[y][5], z[y][6], z[y][7]};
         }
       }
       // the entering state's part of the outputs
@@ -358,19 +369,23 @@ __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(At
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = st[m / 2][m % 2 * 8 + e];
-        bf16 hi[8];
-        take_part(x, hi);
-        const b16x8 sh = as_vector(hi), sl = round_all(x);
+        b16x8 w[kParts];
+        parts_of(x, w);
         const bf16 *s = s_q + l32 * kLdA + part * (kA / P) + m * 16 + half * 4;
         const b16x8 q0 = read_both(s, s + 8), q1 = read_both(s + 32 * kLdA, s + 32 * kLdA + 8);
-        o[0] = mfma32(sh, q0, o[0]);
-        o[1] = mfma32(sh, q1, o[1]);
-        o[0] = mfma32(sl, q0, o[0]);
-        o[1] = mfma32(sl, q1, o[1]);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+          o[0] = mfma32(w[i], q0, o[0]);
+          o[1] = mfma32(w[i], q1, o[1]);
+        }
         if constexpr (kIn == 2) {
           const bf16 *r = s + kPlaneA;
-          o[0] = mfma32(sh, read_both(r, r + 8), o[0]);
-          o[1] = mfma32(sh, read_both(r + 32 * kLdA, r + 32 * kLdA + 8), o[1]);
+          const b16x8 r0 = read_both(r, r + 8), r1 = read_both(r + 32 * kLdA, r + 32 * kLdA + 8);
+#pragma unroll
+          for (int i = 0; i < kParts - 1; ++i) {
+            o[0] = mfma32(w[i], r0, o[0]);
+            o[1] = mfma32(w[i], r1, o[1]);
+          }
         }
       }
       if constexpr (P == 1) {
@@ -404,13 +419,7 @@ __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(At
         x[e] = y * (e < 4 ? w0[e & 3] : w1[e & 3]);
       }
       b16x8 w[kParts];
-#pragma unroll
-      for (int i = 0; i < kParts - 1; ++i) {
-        bf16 y[8];
-        take_part(x, y);
-        w[i] = as_vector(y);
-      }
-      w[kParts - 1] = round_all(x);
+      parts_of(x, w);
 #pragma unroll
       for (int z = 0; z < kIn; ++z) {
         b16x8 kt[SB];
@@ -440,14 +449,20 @@ __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(At
 #pragma unroll
       for (u32 jb = 0; jb < 4; ++jb) {
         if (P == 2 && jb >= 2 + 2 * part) break;
+        b16x8 vq[kIn];
 #pragma unroll
-        for (int z = 0; z < kIn; ++z) {
-          const b16x8 vq = values(jb, z);
+        for (int z = 0; z < kIn; ++z) vq[z] = values(jb, z);
 #pragma unroll
-          for (u32 x = P == 2 ? 0 : jb / 2; x < kOwn; ++x)
+        for (u32 x = P == 2 ? 0 : jb / 2; x < kOwn; ++x) {
+          const f32x4 *p = reinterpret_cast<const f32x4 *>(s_p + (((part + x) * 2 + jb) * kWave + lane) * 8);
+          const f32x4 p0 = p[0], p1 = p[1];
+          float y[8] = {p0[0], p0[1], p0[2], p0[3], p1[0], p1[1], p1[2], p1[3]};
+          b16x8 w[kParts];
+          parts_of(y, w);
 #pragma unroll
-            for (int i = 0; i < 2 - z; ++i)
-              o[x] = mfma32(vq, *reinterpret_cast<const b16x8 *>(s_p[i] + (((part + x) * 2 + jb) * kWave + lane) * 8), o[x]);
+          for (int z = 0; z < kIn; ++z)
+#pragma unroll
+            for (int i = 0; i < kParts - z; ++i) o[x] = mfma32(vq[z], w[i], o[x]);
         }
       }
       // lane (l32, half): a query, columns 8 y + 4 half .. + 3 of the block's 32
@@ -491,37 +506,37 @@ __global__ __launch_bounds__(P * NW * kWave, AB <= 4 ? 2 : 1) void k_attend16(At
   }
 }
 
-template <class T, int AB, int NW, int P, bool OUT, bool EXACT>
+template <class T, int AB, int NW, int P, bool OUT>
 void launch(const AttendJobs &l, bool fast, hipStream_t s) {
-  if (fast) hipLaunchKernelGGL((k_attend16<T, AB, NW, P, OUT, EXACT, true>), grid_of(l), dim3(P * NW * kWave), 0, s, l);
-  else hipLaunchKernelGGL((k_attend16<T, AB, NW, P, OUT, EXACT, false>), grid_of(l), dim3(P * NW * kWave), 0, s, l);
+  if (fast) hipLaunchKernelGGL((k_attend16<T, AB, NW, P, OUT, true>), grid_of(l), dim3(P * NW * kWave), 0, s, l);
+  else hipLaunchKernelGGL((k_attend16<T, AB, NW, P, OUT, false>), grid_of(l), dim3(P * NW * kWave), 0, s, l);
 }
 
 // Two waves for each block of columns shorten a chunk but take the weighted values apart
 // twice: they are for workgroups that have a compute unit to themselves, because
 // there are few or because no two fit its LDS (float16 with more than 64 rows or
-// columns), for two on one (64 x 64, bfloat16), and for two waves with 128 rows,
+// columns), for two on one (64 x 64, bfloat16), and for 64 columns with 128 or 256 rows,
 // whose registers leave a lane no other wave.  In us a chunk of 64, one wave and two:
 //   workgroups for each compute unit    1           2           3           4
-//   bfloat16  64 x 64                2.7, 2.3    3.9, 3.2    4.8, 6.0    7.0, 7.3
-//            128 x 64                  -, 3.0    5.2, 4.4    9.5, 7.2   10.5, 9.3
-//             64 x 128                 -, 3.2    5.1, 6.5    7.6, 9.9    9.5, 12.7
-//            128 x 128               3.9, 3.8    7.0, 8.0   10.7, 12.5  14.1, 16.2
-//   float16   64 x 64                5.2, 3.9    5.3, 7.2    9.8, 10.4  10.1, 13.7
-//            128 x 128               6.9, 6.0
+//   bfloat16  64 x 64                3.3, 2.7    4.8, 3.9    5.1, 5.7    6.0, 7.1
+//            128 x 64                5.1, 3.2    5.5, 4.9   10.0, 7.7   10.4, 9.8
+//            256 x 64               12.8, 5.6   29.0, 10.9
+//             64 x 128               3.3, 3.3    5.5, 6.8    8.3, 9.5   10.4, 13.4
+//            128 x 128               4.3, 4.3    7.8, 8.5   11.8, 12.6  15.2, 16.6
+//   float16   64 x 64                5.4, 3.9    5.7, 7.6   11.1, 11.4  11.1, 15.2
+//            128 x 64                8.1, 5.4
+//             64 x 128               5.4, 4.7
+//            128 x 128               7.3, 6.7
+// (The three gradients of 128 x 128 states, 192 workgroups: 410 us with training's
+// other launches, 403 with two waves.)
 template <class T, int AB, int NW>
-void launch(const AttendJobs &l, bool out, bool exact, bool fast, hipStream_t s) {
-  constexpr bool kHalf = std::is_same<T, f16>::value, kAll = AB == 4 && NW == 2 || kHalf && (AB == 4 || NW == 4);
-  if (!out) return launch<T, AB, NW, 1, false, true>(l, fast, s);
-  if constexpr (AB <= 4)
-    if (kAll || grid_of(l).x <= (!kHalf && NW == 2 ? 2 : 1) * (u32)compute_units()) {
-      if (exact) return launch<T, AB, NW, 2, true, true>(l, fast, s);
-      return launch<T, AB, NW, 2, true, false>(l, fast, s);
-    }
-  if constexpr (!kAll) {
-    if (exact) launch<T, AB, NW, 1, true, true>(l, fast, s);
-    else launch<T, AB, NW, 1, true, false>(l, fast, s);
-  }
+void launch(const AttendJobs &l, bool out, bool fast, hipStream_t s) {
+  constexpr bool kHalf = std::is_same<T, f16>::value, kAll = AB >= 4 && NW == 2 || kHalf && (AB == 4 || NW == 4);
+  if (!out) return launch<T, AB, NW, 1, false>(l, fast, s);
+  if constexpr (AB <= 4 || kAll)
+    if (kAll || grid_of(l).x <= (!kHalf && NW == 2 ? 2 : 1) * (u32)compute_units())
+      return launch<T, AB, NW, 2, true>(l, fast, s);
+  if constexpr (!kAll) launch<T, AB, NW, 1, true>(l, fast, s);
 }
 
 bool fast_view(const View &v) { return v.vec == 8 && v.pos >= 0 && v.pos < (1 << 23); }
@@ -532,7 +547,7 @@ void attend_all(const AttendJobs &jobs, bool out, hipStream_t s) {
   // (sweeps of another kernel, or with other needs, have launches of their own)
   auto kind = [&](const AttendArgs &a) {
     const bool fast = (!out || (fast_view(a.q) && a.W % 8 == 0)) && fast_view(a.k) && fast_view(a.v);
-    return padded_dim(a.A) * 8 + (a.W <= 64 ? 0 : 4) + (fast ? 2 : 0) + (a.end.p ? 1 : 0);
+    return padded_dim(a.A) * 4 + (a.W <= 64 ? 0 : 2) + (fast ? 1 : 0);
   };
   auto tiles = [](const AttendArgs &a) { return (u32)ceil_div(a.W, columns16(a.W)); };
   for (u32 i = 0; i < jobs.jobs;) {
@@ -542,16 +557,16 @@ void attend_all(const AttendJobs &jobs, bool out, hipStream_t s) {
     l.jobs = 0;
     for (; i < jobs.jobs && kind(jobs.j[i]) == first && tiles(jobs.j[i]) == l.col_tiles; ++i)
       l.j[l.jobs++] = jobs.j[i];
-    const bool fast = first & 2, exact = first & 1;
-    const u32 A = first / 8;
-    if (first & 4) {
-      if (A == 64) launch<T, 2, 4>(l, out, exact, fast, s);
-      else if (A == 128) launch<T, 4, 4>(l, out, exact, fast, s);
-      else if constexpr (kWide) launch<T, 8, 4>(l, out, exact, fast, s);
+    const bool fast = first & 1;
+    const u32 A = first / 4;
+    if (first & 2) {
+      if (A == 64) launch<T, 2, 4>(l, out, fast, s);
+      else if (A == 128) launch<T, 4, 4>(l, out, fast, s);
+      else if constexpr (kWide) launch<T, 8, 4>(l, out, fast, s);
     } else {
-      if (A == 64) launch<T, 2, 2>(l, out, exact, fast, s);
-      else if (A == 128) launch<T, 4, 2>(l, out, exact, fast, s);
-      else if constexpr (kWide) launch<T, 8, 2>(l, out, exact, fast, s);
+      if (A == 64) launch<T, 2, 2>(l, out, fast, s);
+      else if (A == 128) launch<T, 4, 2>(l, out, fast, s);
+      else if constexpr (kWide) launch<T, 8, 2>(l, out, fast, s);
     }
   }
 }

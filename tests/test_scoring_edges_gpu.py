@@ -318,3 +318,82 @@ def test_attention_of_many_short_rows(S):
     o, f = S.linear_attention(*many, ld, initial_state=s1)
     assert torch.equal(o.view(-1, *out.shape), out.expand(B // few, *out.shape))
     assert torch.equal(f.view(-1, *final.shape), final.expand(B // few, *final.shape))
+
+
+HALF16 = ["bfloat16", "float16"]
+
+
+@pytest.mark.parametrize("dtype", HALF16)
+@pytest.mark.parametrize("B,T,dk,dv", [(1, 2, 8, 8), (3, 40, 64, 64), (1, 70, 48, 80), (2, 9, 128, 128),
+                                       (600, 2, 64, 64), (2, 3, 200, 40)])
+def test_attention_scores_that_cancel(S, B, T, dk, dv, dtype):
+    """Scores of more than 16 digits whose values cancel: whole numbers, exact in 32-bit sums."""
+    import torch
+    g = gen(70 + dk)
+    few = 8  # elements that are not zero: every sum stays below 2^24
+    big, small = (255, 127) if dtype == "bfloat16" else (2047, 500)
+    q, k = (torch.zeros(B, T, 1, dk, device="cuda") for _ in range(2))
+    at = torch.randperm(dk, generator=g, device="cuda")[:few]
+    q[..., at] = torch.randint(1, small, (B, T, 1, few), generator=g, device="cuda").float()
+    k[..., at] = torch.randint(big // 2, big, (B, T, 1, few), generator=g, device="cuda").float()
+    # position 1's key is position 0's but for one, and its value the negative
+    k[:, 1] = k[:, 0]
+    k[:, 1, :, at[3]] += 1
+    v = torch.zeros(B, T, 1, dv, device="cuda")
+    v[:, 0], v[:, 1] = 1.0, -1.0
+    dt = getattr(torch, dtype)
+    for x in (q, k, v):
+        assert torch.equal(x, x.to(dt).float())
+    out, _ = S.linear_attention(*(x.to(dt) for x in (q, k, v)), torch.zeros(1, device="cuda"))
+    want = -(q[:, 1:, :, at[3]])
+    assert torch.equal(want, want.to(dt).float())
+    assert torch.equal(out[:, 1:].float(), want[..., None].expand(B, T - 1, 1, dv))
+
+
+@pytest.mark.parametrize("dtype", HALF16)
+@pytest.mark.parametrize("B,T,dk,dv", [(1, 1, 8, 8), (3, 70, 64, 64), (2, 9, 128, 128), (1, 131, 48, 80),
+                                       (600, 2, 64, 64), (2, 3, 200, 40)])
+def test_attention_states_that_cancel(S, B, T, dk, dv, dtype):
+    """Whole numbers of 23 digits in the entering state, of which the outputs see the
+    difference of two."""
+    import torch
+    g = gen(71 + dk)
+    s0 = torch.randint(1 << 22, (1 << 23) - 256, (B, 1, dk, dv), generator=g, device="cuda").float()
+    d = torch.randint(-120, 120, (B, 1, dv), generator=g, device="cuda").float()
+    s0[:, :, 1] = s0[:, :, dk - 1] + d
+    q = torch.zeros(B, T, 1, dk, device="cuda")
+    q[..., 1], q[..., dk - 1] = 1.0, -1.0
+    z = torch.zeros(B, T, 1, max(dk, dv), device="cuda")
+    dt = getattr(torch, dtype)
+    out, final = S.linear_attention(q.to(dt), z[..., :dk].to(dt), z[..., :dv].to(dt),
+                                    torch.zeros(1, device="cuda"), initial_state=s0)
+    assert torch.equal(final, s0)
+    assert torch.equal(out.float(), d[:, None].expand(B, T, 1, dv))
+
+
+@pytest.mark.parametrize("dtype", HALF16)
+@pytest.mark.parametrize("d", [48, 64])
+@pytest.mark.parametrize("T", [130, 4000])
+def test_attention_decayed_values_that_cancel(S, d, T, dtype):
+    """Two positions whose decayed values cancel to a thousandth, seen 69 positions and a
+    chunk later.  What is rounded on the way: the decays' powers, a value's weight, the state (twice), its
+    factor in the output: 16 units of 2^-24 of the terms at most."""
+    import torch
+    g = gen(72 + d)
+    H = 48
+    dt = getattr(torch, dtype)
+    a = (1 + torch.rand(H, generator=g, device="cuda")).to(dt)
+    b = (a.float() * 0.985).to(dt)
+    ld = (torch.log(b.double() / a.double()) + 1e-3).float()
+    q, k, v = (torch.zeros(1, T, H, d, device="cuda", dtype=dt) for _ in range(3))
+    k[:, :2, :, 5] = 1
+    q[..., 5] = 1
+    v[:, 0] = a[None, :, None]
+    v[:, 1] = -b[None, :, None]
+    out, _ = S.linear_attention(q, k, v, ld)
+    A, Bv, L = (R.f64(x) for x in (a, b, ld))
+    for t in (66, 70, 127, 129):
+        want = np.exp(L * t) * A - np.exp(L * (t - 1)) * Bv
+        mag = np.exp(L * t) * A + np.exp(L * (t - 1)) * Bv
+        bound = R.HALF[dtype] * 1.01 * np.abs(want) + 16 * R.U32 * mag + R.TINY[dtype]
+        near(out[0, t], np.repeat(want[:, None], d, 1), bound[:, None], f"position {t}")
