@@ -397,3 +397,107 @@ def test_attention_decayed_values_that_cancel(S, d, T, dtype):
         mag = np.exp(L * t) * A + np.exp(L * (t - 1)) * Bv
         bound = R.HALF[dtype] * 1.01 * np.abs(want) + 16 * R.U32 * mag + R.TINY[dtype]
         near(out[0, t], np.repeat(want[:, None], d, 1), bound[:, None], f"position {t}")
+
+
+def dense(q, k, v, ld, scale, s0, n):
+    """out and final state from the whole masked, decayed score matrix."""
+    import torch
+    T = q.shape[1]
+    q, k, v = (x.transpose(1, 2) for x in (q, k, v))
+    at = torch.arange(T, dtype=torch.float64, device=q.device)
+    n = torch.full((q.shape[0],), T, device=q.device) if n is None else n
+    n = n.double().view(-1, 1, 1, 1)
+    live = (at.view(1, 1, T, 1) < n).double()
+    k, v = k * live, v * live
+    g = ld.view(1, -1, 1, 1)
+    gap = at[:, None] - at[None, :]
+    scores = q @ k.transpose(2, 3).contiguous() * (torch.exp(g * gap.clamp(min=0)) * (gap >= 0))
+    reach = torch.exp(g * (at.view(1, 1, T, 1) + 1))
+    out = scale * live * (scores @ v + reach * (q @ s0))
+    left = torch.exp(g * (n - 1 - at.view(1, 1, T, 1)).clamp(min=0))
+    return out.transpose(1, 2), (k * left).transpose(2, 3).contiguous() @ v + torch.exp(g * n) * s0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("B,T,H,dk,dv", [(48, 70, 16, 64, 64), (48, 70, 16, 64, 128), (48, 70, 16, 48, 80),
+                                         (48, 67, 16, 33, 65), (48, 70, 16, 128, 128),
+                                         (40, 70, 13, 128, 64), (9, 70, 5, 200, 32), (9, 70, 5, 32, 200),
+                                         (40, 70, 16, 256, 200)])
+def test_attention_of_many_rows(S, B, T, H, dk, dv, dtype):
+    """More rows and heads than compute units, of every width, against the whole score matrix in 64
+    bits; gradients against that form's own."""
+    import torch
+    g = gen(80 + dk + dv)
+    q, k, v = (normal(g, B, T, H, d, dtype=dtype).requires_grad_() for d in (dk, dk, dv))
+    ld = -torch.exp(torch.empty(H, device="cuda").uniform_(-7, 0, generator=g))
+    s0 = normal(g, B, H, dk, dv).requires_grad_()
+    n = torch.randint(0, T + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    n[0], n[1] = T, 0
+    scale = float(np.float32(dk ** -0.5))
+    out, final = S.linear_attention(q, k, v, ld, scale=scale, initial_state=s0, lengths=n)
+    do, ds = normal(g, *out.shape, dtype=dtype), normal(g, *final.shape)
+    got = [out, final, *torch.autograd.grad((out, final), (q, k, v, s0), (do, ds))]
+    found = []
+    for magnitude in (False, True):
+        x = [y.detach().double() for y in (q, k, v, s0, do, ds)]
+        if magnitude:
+            x = [y.abs() for y in x]
+        for y in x[:4]:
+            y.requires_grad_()
+        o, f = dense(*x[:3], ld.double(), scale, x[3], n)
+        found.append([o.detach(), f.detach(), *torch.autograd.grad((o, f), x[:4], x[4:])])
+    terms = (dk + dv + 2 * T + 64) * R.U32
+    for name, a, w, m in zip(("out", "final", "dq", "dk", "dv", "dinit"), got, *found):
+        t = str(a.dtype).replace("torch.", "")
+        assert a.shape == w.shape and torch.isfinite(a).all(), name
+        off = (a.double() - w).abs() - (R.HALF[t] * 1.01 * w.abs() + terms * m + R.TINY[t])
+        assert off.max() <= 0, f"{name}: {float(off.max()):.3g} beyond what is allowed"
+
+
+def test_calls_from_several_threads(S):
+    """Calls of four threads, each on a stream of its own, give what they give alone."""
+    import threading
+    import torch
+    g = gen(90)
+    w = normal(g, 300, 64)
+    ld = -torch.rand(2, generator=g, device="cuda")
+    work = []
+    for i in range(4):
+        t = labels_of(g, (2000 + i,), 300)
+        x = normal(g, 40, 1000 + i, dtype="bfloat16")
+        q = normal(g, 2, 200 + i, 2, 64, dtype="bfloat16")
+        go = normal(g, 2000 + i, 64)
+        work.append((t, x, q, go))
+
+    def run(t, x, q, go):
+        a = w.detach().requires_grad_()
+        e = S.embed(a, t)
+        o, s = S.linear_attention(q, q, q, ld)
+        return [e.detach(), *torch.autograd.grad(e, a, go), o, s,
+                S.label_logprob(x, t[:40] % 1000), S.linear_attention_step(q[:, 0], q[:, 1], q[:, 2], ld, s)[0]]
+
+    want = [run(*a) for a in work]
+    torch.cuda.synchronize()
+    found, failed = [None] * 4, []
+
+    def body(i):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for _ in range(10):
+                    found[i] = run(*work[i])
+                    with pytest.raises(Exception, match=f"\\({i + 7},"):
+                        S.label_logprob(work[i][1][:, :3], torch.zeros(i + 7, dtype=torch.int32, device="cuda"))
+                s.synchronize()
+        except BaseException as e:  # noqa: B036 (told by the thread that waits)
+            failed.append((i, repr(e)))
+
+    threads = [threading.Thread(target=body, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for a, b in zip(want, found):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
