@@ -422,7 +422,8 @@ def dense(q, k, v, ld, scale, s0, n):
 @pytest.mark.parametrize("B,T,H,dk,dv", [(48, 70, 16, 64, 64), (48, 70, 16, 64, 128), (48, 70, 16, 48, 80),
                                          (48, 67, 16, 33, 65), (48, 70, 16, 128, 128),
                                          (40, 70, 13, 128, 64), (9, 70, 5, 200, 32), (9, 70, 5, 32, 200),
-                                         (40, 70, 16, 256, 200)])
+                                         (40, 70, 16, 256, 200), (9, 70, 5, 201, 33),
+                                         (33, 70, 16, 100, 33), (3, 70, 5, 255, 129)])
 def test_attention_of_many_rows(S, B, T, H, dk, dv, dtype):
     """More rows and heads than compute units, of every width, against the whole score matrix in 64
     bits; gradients against that form's own."""
