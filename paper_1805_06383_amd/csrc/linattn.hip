@@ -492,12 +492,12 @@ struct Plan {
     double alone = 4.0, each = 2.7 * wide / 64;
     u32 resident = wide > 128 ? 1 : wide > 64 ? 2 : 3;
     if (half && a.dtype == FSTC_F16) {
-      alone = large ? 0.0 : 2.35;
-      each = large == 2 ? 6.1 : large ? 4.6 : 1.5;
+      alone = large ? 0.0 : 2.2;
+      each = large == 2 ? 6.7 : large ? 5.1 : 1.75;
       resident = large ? 1 : 2;
     } else if (half) {
-      alone = large == 2 ? 0.3 : large ? 1.2 : 0.9;
-      each = large == 2 ? 3.45 : large ? 1.8 : 1.4;
+      alone = large == 2 ? 0.8 : 1.3;
+      each = large == 2 ? 3.5 : large ? 1.95 : 1.2;
       resident = large ? 2 : 4;
     }
     auto chunk_time = [&](u64 groups) {
@@ -533,7 +533,7 @@ struct Plan {
     if (!direct) state_bytes = ((u64)a.batch * a.heads * segments * rows * cols * sizeof(float) + 255) & ~255ull;
   }
 
-  static constexpr u64 kComputeUnits = 256;
+  static constexpr u64 kComputeUnits = 256;  // (not asked for: a workspace's size needs no device)
   static constexpr u64 kMostGroups = 8 * kComputeUnits;
   static constexpr double kStatePass = 0.45;  // of the sweep proper's time
   static constexpr double kLaunches = 14;     // of two more launches, us
