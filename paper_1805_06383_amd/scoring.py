@@ -55,8 +55,7 @@ def _values(name: str, x, ndim: int, like: torch.Tensor | None = None) -> int:
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
-    """x itself where its last dimension is consecutive and no element is met
-    twice by accident of a negative step, else a contiguous copy."""
+    """x itself where its last dimension is consecutive, else a contiguous copy."""
     return x if x.stride(-1) == 1 or x.shape[-1] <= 1 else x.contiguous()
 
 
