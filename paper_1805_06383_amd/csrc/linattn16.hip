@@ -16,8 +16,8 @@
 // (4.5 TB/s) after 41 us of segment states; 4 x 4,096 positions of 16 heads, 128 x 128
 // states, 85 us for 268 MB in eight segments, and 290 to 335 us for the three gradients
 // in one segment, 192 workgroups of which each has a compute unit to itself:
-// 4.3 us a chunk, of which the vector, the matrix and the LDS units are busy 68%, 42%
-// and 42%, in turn.
+// 4.5 to 5.2 us a chunk, of which the vector, the matrix and the LDS units are busy 68%,
+// 42% and 42%, in turn.
 //
 // A lane's eight elements of a contraction are those that a result gives it
 // (32 x 32: rows 4 h + r and 8 + 4 h + r of each 16, h = lane / 32).  The
