@@ -132,7 +132,7 @@ class _Embed(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad):
         _first_derivatives_only(grad)
-        (labels,) = ctx.saved_tensors
+        labels = ctx.saved_tensors[0].contiguous()
         (rows, dim), n = ctx.shape, labels.numel()
         grad = _rows(grad.reshape(n, dim))
         if n and grad.stride(0) < dim:  # a broadcast gradient
@@ -207,7 +207,10 @@ class _LinearAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout, dfinal):
         _first_derivatives_only(dout, dfinal)
-        q, k, v, log_decay, init, lengths = ctx.saved_tensors
+        # (hooks may give back what was saved laid out otherwise)
+        q, k, v, *rest = ctx.saved_tensors
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        log_decay, init, lengths = (x if x is None else x.contiguous() for x in rest)
         if dout is None:
             dout = torch.zeros((), dtype=q.dtype, device=q.device).expand(*q.shape[:3], v.shape[3])
         dout = _rows(dout)
@@ -330,6 +333,14 @@ def _logit_rows(logits):
     return x, x.shape[0], vocab, max(x.stride(0), vocab)
 
 
+def _saved_logits(ctx):
+    """Logits that a forward pass kept, their rows, the labels and the rows' statistics (hooks
+    may give them back laid out otherwise, so the rows are measured again)."""
+    x, labels, kept = ctx.saved_tensors
+    x, *rows = _logit_rows(x)
+    return x, rows, labels.contiguous(), kept.contiguous()
+
+
 def _logprob_forward(x, n, vocab, stride, labels, size, extra=0):
     """Log-probabilities, and a buffer that starts with what the gradient needs of each
     row (2 n values) and has `extra` more."""
@@ -351,8 +362,8 @@ def _logprob_grad(shape, x, n, vocab, stride, labels, size, kept, weight, per, f
 class _LabelLogprob(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, size):
-        x, *ctx.rows = _logit_rows(logits)
-        lp, kept = _logprob_forward(x, *ctx.rows, labels, size)
+        x, *rows = _logit_rows(logits)
+        lp, kept = _logprob_forward(x, *rows, labels, size)
         ctx.save_for_backward(x, labels, kept)
         ctx.size, ctx.shape = size, logits.shape
         return lp
@@ -360,9 +371,9 @@ class _LabelLogprob(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad):
         _first_derivatives_only(grad)
-        x, labels, kept = ctx.saved_tensors
+        x, rows, labels, kept = _saved_logits(ctx)
         grad = grad.contiguous()
-        return _logprob_grad(ctx.shape, x, *ctx.rows, labels, ctx.size, kept, grad.data_ptr(), 1,
+        return _logprob_grad(ctx.shape, x, *rows, labels, ctx.size, kept, grad.data_ptr(), 1,
                              None), None, None
 
 
@@ -397,9 +408,8 @@ def _preference_forward(x, n, vocab, stride, labels, size, ref, beta, smoothing)
 class _Preference(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, size, ref, beta, smoothing):
-        x, *ctx.rows = _logit_rows(logits)
-        kept, loss, seq, margin = _preference_forward(x, *ctx.rows, labels, size, ref, beta,
-                                                      smoothing)
+        x, *rows = _logit_rows(logits)
+        kept, loss, seq, margin = _preference_forward(x, *rows, labels, size, ref, beta, smoothing)
         ctx.save_for_backward(x, labels, kept)
         ctx.size, ctx.shape = size, logits.shape
         ctx.mark_non_differentiable(seq, margin)
@@ -409,9 +419,9 @@ class _Preference(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad, _seq, _margin):
         _first_derivatives_only(grad)
-        x, labels, kept = ctx.saved_tensors
-        return _logprob_grad(ctx.shape, x, *ctx.rows, labels, ctx.size, kept,
-                             kept.data_ptr() + 8 * ctx.rows[0], max(1, labels.shape[1]),
+        x, rows, labels, kept = _saved_logits(ctx)
+        return _logprob_grad(ctx.shape, x, *rows, labels, ctx.size, kept,
+                             kept.data_ptr() + 8 * rows[0], max(1, labels.shape[1]),
                              grad.data_ptr()), None, None, None, None, None
 
 

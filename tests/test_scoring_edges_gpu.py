@@ -502,3 +502,44 @@ def test_calls_from_several_threads(S):
     for a, b in zip(want, found):
         for x, y in zip(a, b):
             assert torch.equal(x, y)
+
+
+def test_saved_tensors_in_another_layout(S):
+    """What a backward pass has kept may come back laid out otherwise (moved to the host and back, or
+    as a hook left it): the gradients are the same, by bits."""
+    import contextlib
+    import torch
+    g = gen(68)
+    wide = normal(g, 4, 3, 2000, dtype="bfloat16")
+    t = labels_of(g, (4, 3), 900)
+    ref = normal(g, 4)
+    qkv = normal(g, 2, 70, 3, 2, 64, dtype="bfloat16")
+    s0 = normal(g, 2, 2, 64, 64)
+    ld = -torch.rand(2, generator=g, device="cuda")
+    n = torch.tensor([70, 33], dtype=torch.int32, device="cuda")
+    w = normal(g, 900, 20)
+
+    def turned(x):
+        if x.ndim >= 2:
+            return x.transpose(0, -1).contiguous().transpose(0, -1)
+        return torch.stack([x, x], -1)[..., 0] if x.ndim else x
+
+    def grads():
+        x = wide[:, :, 7:907].detach().requires_grad_()
+        q, k, v = (y.detach().requires_grad_() for y in qkv.unbind(2))
+        i = s0.detach().requires_grad_()
+        a = w.detach().requires_grad_()
+        o, f = S.linear_attention(q, k, v, ld, initial_state=i, lengths=n)
+        return [lambda: torch.autograd.grad(S.label_logprob(x, t).sum(), x),
+                lambda: torch.autograd.grad(S.preference_loss(x, t, ref)[0], x),
+                lambda: torch.autograd.grad(o.float().sum() + f.sum(), (q, k, v, i)),
+                lambda: torch.autograd.grad(S.embed(a, t).square().sum(), a)]
+
+    found = []
+    for hooks in (contextlib.nullcontext(), torch.autograd.graph.save_on_cpu(),
+                  torch.autograd.graph.saved_tensors_hooks(lambda x: x, turned)):
+        with hooks:
+            found.append([y for f in grads() for y in f()])
+    for other in found[1:]:
+        for a, b in zip(found[0], other):
+            assert torch.equal(a, b)
