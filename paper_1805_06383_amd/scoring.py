@@ -256,7 +256,9 @@ def linear_attention(q, k, v, log_decay, scale: float = 1.0, initial_state=None,
     (None: zero), lengths int32 [batch] (None: all positions).  Returns (out,
     final_state): out has q's type, zero at and beyond a row's length;
     final_state is float32, the state after the row's last position, from which
-    linear_attention_step goes on.  Differentiable in q, k, v and initial_state."""
+    linear_attention_step goes on.  Differentiable in q, k, v and initial_state.
+    Nothing beyond a length is read; within it a value that is not finite may reach outputs
+    up to 63 positions before it, as well as all after it, and an infinity may end as NaN."""
     _refuse_lost(q, k, v, log_decay, initial_state)
     q, k, v, log_decay = _attention_inputs(q, k, v, log_decay, 4)
     B, T, H, dk = q.shape
