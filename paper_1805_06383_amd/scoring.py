@@ -94,7 +94,7 @@ def _refuse_lost(*tensors):
         for x in tensors:
             if x is not None and forward_ad.unpack_dual(x).tangent is not None:
                 _refuse("forward-mode derivatives are not available")
-    if torch.jit.is_tracing():
+    if torch._C._is_tracing():
         _refuse("the operators cannot be traced")
 
 
@@ -435,9 +435,8 @@ def preference_loss(logits: torch.Tensor, labels: torch.Tensor, ref_logprob: tor
     labels outside the vocabulary): sequence p of the first half is preferred to
     sequence pairs + p.  ref_logprob float32 [2 * pairs]: the sequences'
     log-probabilities under a reference model (sums of label_logprob), which is fixed
-    (no gradient).  Returns
-    (loss, logprob [2 * pairs], margin [pairs]), float32: with L the sequences'
-    log-probabilities, margin = beta * ((L - ref) of the preferred - (L - ref) of
+    (no gradient).  Returns (loss, logprob [2 * pairs], margin [pairs]), float32: with
+    L the sequences' log-probabilities, margin = beta * ((L - ref) of the preferred - (L - ref) of
     the other), loss = mean of -(1 - label_smoothing) log sigmoid(margin) -
     label_smoothing log sigmoid(-margin).  A sequence with a label of logit -inf has
     log-probability -inf and its pair an infinite margin; where infinities cancel
