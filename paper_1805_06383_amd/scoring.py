@@ -37,6 +37,7 @@ __all__ = ["embed", "label_logprob", "linear_attention", "linear_attention_step"
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _LABEL_BYTES = {torch.int32: 4, torch.int64: 8}
 _I64x3 = ctypes.c_int64 * 3
+_PROXY = torch._C._TorchDispatchModeKey.PROXY  # (of a trace by torch.fx)
 
 
 def _refuse(msg: str):
@@ -94,7 +95,7 @@ def _refuse_lost(*tensors):
         for x in tensors:
             if x is not None and forward_ad.unpack_dual(x).tangent is not None:
                 _refuse("forward-mode derivatives are not available")
-    if torch._C._is_tracing():
+    if torch._C._is_tracing() or torch._C._get_dispatch_mode(_PROXY) is not None:
         _refuse("the operators cannot be traced")
 
 

@@ -243,6 +243,15 @@ def test_tracing_is_refused(S):
         f(*inputs)
 
 
+def test_tracing_by_fx_is_refused(S):
+    from torch.fx.experimental.proxy_tensor import make_fx
+    from paper_1805_06383_amd.fstc import FstcError
+    for name, f, inputs in calls_of(S):
+        with pytest.raises(FstcError, match="trace"):
+            make_fx(f)(*inputs)
+        f(*inputs)
+
+
 def test_a_reference_that_wants_a_gradient_is_refused(S):
     import torch
     from paper_1805_06383_amd.fstc import FstcError
